@@ -17,6 +17,7 @@
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
+#include "fp8_scales.h"
 #include "kernels.h"
 #include "oled.h"
 
@@ -182,7 +183,6 @@ constexpr int kTileRows = 256;       // weight rows of a tile (up: 128 features)
 constexpr int kTileThreads = 512;
 constexpr int kTileMaxLd = 1 << 22;  // row stride up to which a tile's offsets stay below 2^31
 constexpr int kBufferFlags = 0x00020000;   // word 3 of a raw buffer resource: 32-bit data
-constexpr int kFarOffset = 0x7FFFFFF0;     // past the end of every buffer: reads zeros
 
 // A weight tile's rows in LDS: within each 32, the order in which lane g of D
 // (rows 4g .. 4g + 3 of two 16-row tiles) holds 8 consecutive features.
@@ -218,6 +218,14 @@ __device__ __forceinline__ void dma16(const u32x4_t& buf, uint32_t to, int off, 
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                :
                : "s"(to), "v"(off), "s"(buf), "s"(add)
+               : "m0", "memory");
+}
+
+// 4 bytes a lane from buffer offset off to LDS at `to` + 4 lane.
+__device__ __forceinline__ void dma4(const u32x4_t& buf, uint32_t to, int off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+               :
+               : "s"(to), "v"(off), "s"(buf)
                : "m0", "memory");
 }
 
@@ -262,14 +270,27 @@ struct Tile {
     else
       wait_loads<N * kFills>();
   }
-  // The scales of 8 stages from stage 8 c on: 32 bytes of each token row, then of
-  // each weight row of blocks.
+  // The scales of 8 stages from stage 8 c on (fewer: those there are): 32 bytes of
+  // each token row, then of each weight row of blocks. The waits for fills do not count
+  // them: what is in flight behind a fill only makes a wait longer.
   __device__ __forceinline__ void fill_scales(uint32_t to, int c) const {
-    if (32 * wave + (lane >> 1) < BN) dma16(sr, to + wave * 1024, soff, 32 * c);
-    if (wave == kWaves - 1 && lane < 4) dma16(vr, to + BN * 32, voff, 32 * c);
+    const int chunk = scale_chunk(c, kb);
+    if (chunk == kWholeChunk) {
+      if (32 * wave + (lane >> 1) < BN) dma16(sr, to + wave * 1024, soff, 32 * c);
+      if (wave == kWaves - 1 && lane < 4) dma16(vr, to + BN * 32, voff, 32 * c);
+    } else if (chunk == kShortChunk) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = __shfl(soff, scale_row_lane(i, lane));
+        if (32 * wave + 8 * i < BN)
+          dma4(sr, to + wave * 1024 + 256 * i, scale_value(row, c, kb, lane));
+      }
+      const int row = __shfl(voff, scale_row_lane(0, lane));
+      if (wave == kWaves - 1 && lane < 16) dma4(vr, to + BN * 32, scale_value(row, c, kb, lane));
+    }
   }
-  // Sets up the fills of an item and weight tile; false: nothing is left to do.
-  __device__ bool place(const F8Args& a, const Item& item, int weight_tile);
+  // Sets up the fills of an item and weight tile whose expert is there.
+  __device__ void place(const F8Args& a, const Item& item, int weight_tile);
 };
 
 __device__ __forceinline__ void read_frag(const uint8_t* __restrict__ p, int o0, u32x4_t (&f)[2]) {
@@ -350,8 +371,30 @@ __device__ __forceinline__ bool pick_tile(const F8Args& a, Item& it, int& tile) 
   }
 }
 
+__device__ __forceinline__ int slot_of(const F8Args& a, int expert) {
+  return a.slot_of ? a.slot_of[expert] : expert;
+}
+
+// Whether this workgroup's expert has no block; its routes' outputs are zeros. (Apart
+// from place(), so that a tile's buffers stay in scalar registers.)
+template <int MODE, int ROWS = kTileRows>
+__device__ __forceinline__ bool absent(const F8Args& a, const Item& it, int tile) {
+  if constexpr (MODE == kPlain) return false;
+  const int slot = slot_of(a, it.expert);
+  if (slot >= 0 && slot < a.n_slots) return false;
+  if constexpr (MODE == kDown) {
+    const int f0 = tile * ROWS;
+    for (int i = threadIdx.x; i < it.rows * (ROWS / 8); i += 2 * ROWS)
+      if (f0 + 8 * (i % (ROWS / 8)) < a.N)
+        *reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(a.out) +
+                                    static_cast<size_t>(it.row0 + i / (ROWS / 8)) * a.ldc + f0 +
+                                    8 * (i % (ROWS / 8))) = u32x4_t{0u, 0u, 0u, 0u};
+  }
+  return true;
+}
+
 template <int MODE, int BN, bool TAIL, int ROWS>
-__device__ __forceinline__ bool Tile<MODE, BN, TAIL, ROWS>::place(const F8Args& a, const Item& item,
+__device__ __forceinline__ void Tile<MODE, BN, TAIL, ROWS>::place(const F8Args& a, const Item& item,
                                                             int weight_tile) {
   it = item;
   tile = weight_tile;
@@ -370,32 +413,22 @@ __device__ __forceinline__ bool Tile<MODE, BN, TAIL, ROWS>::place(const F8Args& 
     wbytes = (rows - 1) * static_cast<int>(a.ldw) + a.K;
     vbase = a.ws + static_cast<int64_t>(f0 / 128) * kb;
     vbytes = (rows + 127) / 128 * kb * 4;
-    voff = min(lane >> 1, (rows - 1) / 128) * kb * 4 + 16 * (lane & 1);
+    voff = min(lane >> 1, (rows - 1) / 128) * kb * 4 + scale_piece(lane);
   } else {
-    const int slot = a.slot_of ? a.slot_of[it.expert] : it.expert;
-    if (slot < 0 || slot >= a.n_slots) {   // the routes of an absent expert: zeros
-      if (MODE == kDown)
-        for (int i = threadIdx.x; i < it.rows * (ROWS / 8); i += 64 * kWaves)
-          if (f0 + 8 * (i % (ROWS / 8)) < a.N)
-            *reinterpret_cast<u32x4_t*>(static_cast<uint16_t*>(a.out) +
-                                        static_cast<size_t>(it.row0 + i / (ROWS / 8)) * a.ldc + f0 +
-                                        8 * (i % (ROWS / 8))) = u32x4_t{0u, 0u, 0u, 0u};
-      return false;
-    }
-    const uint8_t* block = a.w + static_cast<int64_t>(slot) * a.slot_bytes;
+    const uint8_t* block = a.w + static_cast<int64_t>(slot_of(a, it.expert)) * a.slot_bytes;
     const int HI = a.H * a.I;
     vbase = reinterpret_cast<const float*>(block + 3 * static_cast<size_t>(HI));
     if constexpr (MODE == kUp) {
       wbase = block;
       wbytes = 2 * HI;
       vbytes = 2 * (HI / 16384) * 4;
-      voff = (min(lane >> 1, 1) * (a.I / 128) + f0 / 128) * kb * 4 + 16 * (lane & 1);
+      voff = (min(lane >> 1, 1) * (a.I / 128) + f0 / 128) * kb * 4 + scale_piece(lane);
     } else {
       wbase = block + 2 * static_cast<size_t>(HI);
       wbytes = HI;
       vbase += 2 * (HI / 16384);
       vbytes = HI / 16384 * 4;
-      voff = min(f0 / 128 + (lane >> 1), a.N / 128 - 1) * kb * 4 + 16 * (lane & 1);
+      voff = min(f0 / 128 + (lane >> 1), a.N / 128 - 1) * kb * 4 + scale_piece(lane);
     }
   }
 #pragma unroll
@@ -439,12 +472,11 @@ __device__ __forceinline__ bool Tile<MODE, BN, TAIL, ROWS>::place(const F8Args& 
     const int c = (lane & 7) ^ ((4 * j + (lane >> 4)) & 7);
     xoff[i] = token(8 * j + (lane >> 3)) * static_cast<int>(a.ldx) + 16 * c;
   }
-  soff = token(32 * wave + (lane >> 1)) * kb * 4 + 16 * (lane & 1);
+  soff = token(32 * wave + (lane >> 1)) * kb * 4 + scale_piece(lane);
   wr = buffer_of(wbase, static_cast<uint32_t>(wbytes));
   xr = buffer_of(xbase, static_cast<uint32_t>(xbytes));
   sr = buffer_of(sbase, static_cast<uint32_t>(sbytes));
   vr = buffer_of(vbase, static_cast<uint32_t>(vbytes));
-  return true;
 }
 
 constexpr int lds_bytes(int bn, int stages) {   // the ring and two buffers of scales
@@ -460,7 +492,7 @@ __device__ __forceinline__ void run_tile(const F8Args& a, const Item& it, int we
   uint8_t (*ring)[TL::kStage] = reinterpret_cast<uint8_t (*)[TL::kStage]>(lds);
   uint8_t (*s_scales)[TL::kScales] = reinterpret_cast<uint8_t (*)[TL::kScales]>(lds + S * TL::kStage);
   TL t;
-  if (!t.place(a, it, weight_tile)) return;
+  t.place(a, it, weight_tile);
   const int f0 = t.f0, kb = t.kb, tile = t.tile;
   const int lane = t.lane, g = lane >> 4, lr = lane & 15;
   const int wm = t.wave >> 2, wn = t.wave & 3;
@@ -650,7 +682,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void k_f8_tile(F8Args a) {
   __shared__ __align__(1024) uint8_t lds[kBytes > kHalfBytes ? kBytes : kHalfBytes];
   Item it;
   int tile;
-  if (!pick_tile<MODE, 64 * NT>(a, it, tile)) return;
+  if (!pick_tile<MODE, 64 * NT>(a, it, tile) || absent<MODE>(a, it, tile)) return;
   if (it.rows <= 64 * kHalf)
     run_tile<MODE, kHalf, 3, TAIL>(a, it, tile, lds);
   else
@@ -686,7 +718,8 @@ __global__ __launch_bounds__(2 * ROWS, ROWS / 64) void k_f8_rows(F8Args a) {
   Item it;
   int tile;
   TL t;
-  if (!pick_tile<MODE, BN, ROWS>(a, it, tile) || !t.place(a, it, tile)) return;
+  if (!pick_tile<MODE, BN, ROWS>(a, it, tile) || absent<MODE, ROWS>(a, it, tile)) return;
+  t.place(a, it, tile);
   const int f0 = t.f0, kb = t.kb, lane = t.lane, wave = t.wave, g = lane >> 4, lr = lane & 15;
 
   floatx4_t acc[2][NT];
@@ -847,11 +880,23 @@ __global__ __launch_bounds__(512) void k_f8_mid(F8Args a) {
   };
   const u32x4_t sbuf = buffer_of(a.xs + static_cast<int64_t>(row0) * kb, static_cast<uint32_t>(rows * kb * 4));
   const u32x4_t vbuf = buffer_of(a.ws + static_cast<int64_t>(f0 / 128) * kb, static_cast<uint32_t>(kb * 4));
-  const int soff = min(32 * (wave & 1) + (lane >> 1), rows - 1) * kb * 4 + 16 * (lane & 1);
+  const int soff = min(32 * (wave & 1) + (lane >> 1), rows - 1) * kb * 4 + scale_piece(lane);
   auto fill_scales = [&](int c) {   // of 8 steps from step 8 c on
     const uint32_t to = lds_addr(s_scales[c & 1]);
-    if (wave < 2) dma16(sbuf, to + 1024 * wave, soff, 32 * c);
-    if (wave == 7 && lane < 2) dma16(vbuf, to + 64 * 32, 16 * lane, 32 * c);
+    const int chunk = scale_chunk(c, kb);
+    if (chunk == kWholeChunk) {
+      if (wave < 2) dma16(sbuf, to + 1024 * wave, soff, 32 * c);
+      if (wave == 7 && lane < 2) dma16(vbuf, to + 64 * 32, scale_piece(lane), 32 * c);
+    } else if (chunk == kShortChunk) {
+      if (wave < 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = __shfl(soff, scale_row_lane(i, lane));
+          dma4(sbuf, to + 1024 * wave + 256 * i, scale_value(row, c, kb, lane));
+        }
+      }
+      if (wave == 7 && lane < 8) dma4(vbuf, to + 64 * 32, scale_value(0, c, kb, lane));
+    }
   };
 
   floatx4_t acc[2][2];
