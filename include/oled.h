@@ -627,7 +627,8 @@ size_t oled_route_scored_workspace(int32_t T, int32_t E);
 
 /*
  * oled_norm_in: the norm in front of a block, n = x rsqrt(mean(x^2) + eps) w,
- *  row by row, sums in fp32. x_dev [T] rows of H in dtype, ldx elements apart;
+ *  row by row, sums in fp32; where mean(x^2) + eps is 0 (a row of zeros, or of values whose
+ *  squares are below fp32, with eps 0) n = 0. x_dev [T] rows of H in dtype, ldx elements apart;
  *  weight_dev [H] fp32, or NULL: the rows as they are (n = x). n_dev [T][H] in
  *  dtype, or NULL; q_dev [T][H] e4m3 of the unrounded n with q_scale_dev
  *  [T][ceil(H / 128)] fp32, or both NULL.
@@ -645,7 +646,8 @@ oled_status oled_norm_in(const void* x_dev, int32_t dtype, int64_t ldx, int32_t 
  *  rounded once to y's dtype. k > 0: f_t = sum_j weights[t][j] f[inv_perm[t k +
  *  j]] over the routes j with inv_perm >= 0 (none: f_t = 0), rows of f in sorted
  *  position as oled_fp8_experts leaves them (f_dev [T*k][H]); k = 0: f_t is row t
- *  of f_dev [T][H], weights_dev and inv_perm_dev are not read.
+ *  of f_dev [T][H], weights_dev and inv_perm_dev are not read. Where mean(f_t^2) +
+ *  eps is 0 the normed row is 0, as it is for a token without routes with any eps.
  *  norm_weight_dev [H] fp32, or NULL: no norm (f_t itself). gate_dev: NULL (1),
  *  or fp32 rows of H: token t takes row t / gate_tokens (row 0 if gate_tokens
  *  is 0). x_dev [T][H] in y_dtype, or NULL (0); y_dev [T][H] may be x_dev.

@@ -85,6 +85,13 @@ __device__ __forceinline__ float row_sum(float v) {
   return v;
 }
 
+// 1 / sqrt(mean square + eps) of a row; 0 where that is 1 / 0 (eps 0 and a row of zeros, a
+// token without routes among them): such a row stays zeros.
+__device__ __forceinline__ float row_factor(float sum, int H, float eps) {
+  const float m = sum / static_cast<float>(H) + eps;
+  return m == 0.f ? 0.f : rsqrtf(m);
+}
+
 struct NormIn {
   const void* x;
   int64_t ldx;
@@ -113,7 +120,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_in(NormIn a) {
     for (int i = 0; i < 8; ++i) ss += v[c][i] * v[c][i];
   }
   if (a.w) {
-    const float r = rsqrtf(row_sum<TPR>(ss) / static_cast<float>(a.H) + a.eps);
+    const float r = row_factor(row_sum<TPR>(ss), a.H, a.eps);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int h = 8 * (sub + TPR * c);
@@ -212,7 +219,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_out(NormOut a) {
     for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss += v[c][i] * v[c][i];
-    const float r = rsqrtf(row_sum<TPR>(ss) / static_cast<float>(a.H) + a.eps);
+    const float r = row_factor(row_sum<TPR>(ss), a.H, a.eps);
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int h = 8 * (sub + TPR * c);
