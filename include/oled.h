@@ -597,8 +597,9 @@ typedef struct {
 /*
  * oled_route_scored: routes T tokens by scores s[e] = 1 / (1 + exp(-l[e])) or
  *  softmax(l)[e], in fp32. An expert's choice value is s[e] + bias[e] (a
- *  balance bias, on the choice alone). Without a bias it is s[e] where group
- *  values are sums, else l[e], which is in the same order. The top_groups
+ *  balance bias, on the choice alone). Without a bias it is s[e] where group_best
+ *  is 2 (also where all groups compete), else l[e], which is in the same order but
+ *  keeps apart what saturated scores do not. The top_groups
  *  groups of the largest values compete, then the k largest choice values, in
  *  falling order; equal ones go to the lower group or expert. weight[t][j] =
  *  scale * s[e_j] / (sum_j s[e_j] + 1e-20), or scale * s[e_j] without renorm.

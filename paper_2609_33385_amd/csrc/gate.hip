@@ -5,16 +5,16 @@
 // batched routing is.
 //
 // Of a token with logits l, scores s = 1 / (1 + exp(-l)), or exp(l - max l) /
-// sum exp(l - max l); choice values c = s + b, or s where only groups need
-// values, or the logits themselves (their order is the scores') where neither
-// does. LPT lanes take a token, G groups of LPT / G lanes, each lane up to EPL
-// experts of one group. A choice value and its expert make one 40-bit key
-// (the ordered bits of c, then 255 - id), held as a double 2^52 + key: a
-// larger key is a larger c or, among equal ones, a lower id, one v_max_f64 or
-// v_min_f64 orders two of them, and no two keys are equal. Each lane sorts its
-// keys into a list of the KP best by a network, and lists merge over lanes:
-// the larger of a[i] and b[KP - 1 - i] are the KP best of both, bitonic, and
-// log2 KP steps sort them.
+// sum exp(l - max l); choice values c = s + b, or s where groups are worth sums of
+// two (also where all groups compete), or the logits themselves (their order is the
+// scores', but for scores that fp32 makes equal) where neither is so. LPT lanes
+// take a token, G groups of LPT / G lanes, each lane up to EPL experts of one
+// group. A choice value and its expert make one 40-bit key (the ordered bits of
+// c, then 255 - id), held as a double 2^52 + key: a larger key is a larger c or,
+// among equal ones, a lower id, one v_max_f64 or v_min_f64 orders two of them,
+// and no two keys are equal. Each lane sorts its keys into a list of the KP best
+// by a network, and lists merge over lanes: the larger of a[i] and b[KP - 1 - i]
+// are the KP best of both, bitonic, and log2 KP steps sort them.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -795,7 +795,7 @@ extern "C" oled_status oled_route_scored(const oled_router* router, const void* 
   a.k = k;
   a.G = G;
   a.top_groups = r.top_groups;
-  a.best = r.top_groups < G ? r.group_best : 1;   // all groups compete: their values do not matter
+  a.best = r.group_best;
   a.softmax = r.score == OLED_SCORE_SOFTMAX;
   a.renorm = r.renorm;
   a.bf16 = r.dtype == OLED_BF16;
