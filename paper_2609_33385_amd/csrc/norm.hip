@@ -101,13 +101,14 @@ struct NormIn {
   void* n;
   uint8_t* q;
   float* qs;
+  uint32_t t0;   // first row of the launch
 };
 
 template <class X, int TPR, int NC>
 __global__ __launch_bounds__(kNormThreads) void k_norm_in(NormIn a) {
-  const int t = blockIdx.x * (kNormThreads / TPR) + static_cast<int>(threadIdx.x) / TPR;
+  const uint32_t t = a.t0 + blockIdx.x * (kNormThreads / TPR) + threadIdx.x / TPR, T = a.T;
   const int sub = threadIdx.x % TPR;
-  const X* row = static_cast<const X*>(a.x) + static_cast<size_t>(min(t, a.T - 1)) * a.ldx;
+  const X* row = static_cast<const X*>(a.x) + static_cast<size_t>(min(t, T - 1)) * a.ldx;
   float v[NC][8];
   float ss = 0.f;
 #pragma unroll
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_in(NormIn a) {
       }
     }
   }
-  if (t >= a.T) return;
+  if (t >= T) return;
   const size_t out = static_cast<size_t>(t) * a.H;
   const int blocks = (a.H + 127) / 128;
 #pragma unroll
@@ -173,15 +174,16 @@ struct NormOut {
   const void* x;
   float alpha;
   void* y;
+  uint32_t t0;   // first token of the launch
 };
 
 // A token's routes in the order of its choice, one row read at a time by all of its
 // threads. Routes without a row add nothing: neither their weight nor a row is read.
 template <class F, class Y, int TPR, int NC>
 __global__ __launch_bounds__(kNormThreads) void k_norm_out(NormOut a) {
-  const int t = blockIdx.x * (kNormThreads / TPR) + static_cast<int>(threadIdx.x) / TPR;
+  const uint32_t t = a.t0 + blockIdx.x * (kNormThreads / TPR) + threadIdx.x / TPR, T = a.T;
   const int sub = threadIdx.x % TPR;
-  const int tt = min(t, a.T - 1);
+  const uint32_t tt = min(t, T - 1);
   const F* f = static_cast<const F*>(a.f);
   float v[NC][8];
 #pragma unroll
@@ -231,14 +233,14 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_out(NormOut a) {
       }
     }
   }
-  if (t >= a.T) return;
+  if (t >= T) return;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const int h = 8 * (sub + TPR * c);
     if (h >= a.H) continue;
     if (a.gate) {
       float g[8];
-      load8(a.gate + static_cast<size_t>(a.gate_tokens ? t / a.gate_tokens : 0) * a.H + h, g);
+      load8(a.gate + static_cast<size_t>(a.gate_tokens ? t / static_cast<uint32_t>(a.gate_tokens) : 0u) * a.H + h, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[c][i] *= g[i];
     }
@@ -253,6 +255,21 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_out(NormOut a) {
   }
 }
 
+// A launch takes fewer than 2^32 threads (the grid of a larger one wraps, without an error):
+// more rows are several launches.
+constexpr int64_t kNormGrid = 1 << 23;
+template <int TPR, int NC, class Fn>
+hipError_t norm_launches(int64_t T, Fn&& launch) {
+  constexpr int64_t rows = kNormThreads / TPR;
+  for (int64_t t0 = 0; t0 < T; t0 += kNormGrid * rows) {
+    const int64_t blocks = (T - t0 + rows - 1) / rows;
+    launch(std::integral_constant<int, TPR>{}, std::integral_constant<int, NC>{}, static_cast<uint32_t>(t0),
+           static_cast<uint32_t>(blocks < kNormGrid ? blocks : kNormGrid));
+    if (hipError_t e = hipGetLastError()) return e;
+  }
+  return hipSuccess;
+}
+
 // Threads of a row and steps by the row's length: a wavefront up to one step, then a
 // workgroup, whose many wavefronts keep more in flight. us, a wavefront against a
 // workgroup, in and out: 16384 x 512 10.2 : 16.3 and 39.6 : 80.8; 16384 x 2048 40.0 : 36.4
@@ -260,19 +277,11 @@ __global__ __launch_bounds__(kNormThreads) void k_norm_out(NormOut a) {
 // 16384 x 4096 82.1 : 67.7 and 313 : 268.
 template <class Fn>
 hipError_t norm_form(int T, int H, Fn&& launch) {
-  using std::integral_constant;
-  if (H <= 512) {
-    launch(integral_constant<int, 64>{}, integral_constant<int, 1>{}, (T + 3) / 4);
-  } else if (H <= 2048) {
-    launch(integral_constant<int, 256>{}, integral_constant<int, 1>{}, T);
-  } else if (H <= 4096) {
-    launch(integral_constant<int, 256>{}, integral_constant<int, 2>{}, T);
-  } else if (H <= 8192) {
-    launch(integral_constant<int, 256>{}, integral_constant<int, 4>{}, T);
-  } else {
-    launch(integral_constant<int, 256>{}, integral_constant<int, 8>{}, T);
-  }
-  return hipGetLastError();
+  if (H <= 512) return norm_launches<64, 1>(T, launch);
+  if (H <= 2048) return norm_launches<256, 1>(T, launch);
+  if (H <= 4096) return norm_launches<256, 2>(T, launch);
+  if (H <= 8192) return norm_launches<256, 4>(T, launch);
+  return norm_launches<256, 8>(T, launch);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -301,10 +310,11 @@ extern "C" oled_status oled_norm_in(const void* x_dev, int32_t dtype, int64_t ld
     set_noctx_error("oled_norm_in: x, weight, n and q must be on 16-byte boundaries");
     return OLED_ERR_INVALID_ARG;
   }
-  const NormIn a{x_dev, ldx, weight_dev, eps, T, H, n_dev, static_cast<uint8_t*>(q_dev), q_scale_dev};
+  NormIn a{x_dev, ldx, weight_dev, eps, T, H, n_dev, static_cast<uint8_t*>(q_dev), q_scale_dev, 0};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const hipError_t e = norm_form(T, H, [&](auto tpr, auto nc, int blocks) {
+  const hipError_t e = norm_form(T, H, [&](auto tpr, auto nc, uint32_t t0, uint32_t blocks) {
     constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
+    a.t0 = t0;
     if (dtype == OLED_F32)
       hipLaunchKernelGGL((k_norm_in<float, TPR, NC>), dim3(blocks), dim3(kNormThreads), 0, s, a);
     else
@@ -343,11 +353,12 @@ extern "C" oled_status oled_norm_out(const void* f_dev, int32_t f_dtype, const f
     set_noctx_error("oled_norm_out: f, norm_weight, gate, x and y must be on 16-byte boundaries");
     return OLED_ERR_INVALID_ARG;
   }
-  const NormOut a{f_dev, weights_dev, inv_perm_dev, k, T, H, norm_weight_dev, eps, gate_dev,
-                  gate_tokens, x_dev, residual_scale, y_dev};
+  NormOut a{f_dev, weights_dev, inv_perm_dev, k, T, H, norm_weight_dev, eps, gate_dev,
+            gate_tokens, x_dev, residual_scale, y_dev, 0};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const hipError_t e = norm_form(T, H, [&](auto tpr, auto nc, int blocks) {
+  const hipError_t e = norm_form(T, H, [&](auto tpr, auto nc, uint32_t t0, uint32_t blocks) {
     constexpr int TPR = decltype(tpr)::value, NC = decltype(nc)::value;
+    a.t0 = t0;
     const dim3 grid(blocks), block(kNormThreads);
     if (f_dtype == OLED_F32) {
       if (y_dtype == OLED_F32)
