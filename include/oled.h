@@ -674,7 +674,8 @@ oled_status oled_norm_out(const void* f_dev, int32_t f_dtype, const float* weigh
  *  of a result of random rows). The same call gives the same bits.
  *  Errors: INVALID_ARG (NULL pointers, M, N or K < 1, lda or ldb < K, ldc < N,
  *  a, b or c off a 16-byte boundary), UNSUPPORTED (K, lda or ldb
- *  not multiples of 16, or lda or ldb above 2^31 - 1).
+ *  not multiples of 16, lda or ldb above 2^31 - 1, or more than 2^23 - 1 tiles, of
+ *  256 features x 128 or 256 rows, or of 16 x 16 where lda or ldb is above 2^22).
  */
 oled_status oled_fp8_matmul(const void* a_dev, const float* a_scale_dev, int64_t lda,
                             const void* b_dev, const float* b_scale_dev, int64_t ldb, int32_t M,

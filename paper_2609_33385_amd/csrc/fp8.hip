@@ -89,6 +89,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {   // v_cvt_p
 
 int64_t tiles(int n, int size) { return (static_cast<int64_t>(n) - 1) / size + 1; }
 
+// A launch takes fewer than 2^32 threads; the grid of a larger one would wrap, without an error.
+bool one_launch(int64_t grid, int64_t threads) { return grid <= static_cast<int64_t>(UINT32_MAX) / threads; }
+
 // ---------------------------------------------------------------------------
 // Small products: a workgroup takes 16 weight rows x 16 token rows, and its 8
 // wavefronts share K: wavefront w takes steps w, w + 8, ... straight into registers,
@@ -160,7 +163,7 @@ __global__ __launch_bounds__(64 * kSplit) void k_f8_split(F8Args a) {
 
 hipError_t launch_split(const F8Args& a, hipStream_t s) {
   const int64_t grid = tiles(a.N, 16) * tiles(a.M, 16);
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  if (!one_launch(grid, 64 * kSplit)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(k_f8_split, dim3(static_cast<uint32_t>(grid)), dim3(64 * kSplit), 0, s, a);
   return hipGetLastError();
 }
@@ -693,7 +696,7 @@ template <int MODE, int NT, int S>
 hipError_t launch_tile(const F8Args& a, int64_t items, hipStream_t s) {
   const int feats = MODE == kUp ? 128 : 256;
   const int64_t grid = items * tiles(a.N, feats);
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  if (!one_launch(grid, kTileThreads)) return hipErrorInvalidConfiguration;
   const dim3 g(static_cast<uint32_t>(grid)), b(kTileThreads);
   if (MODE == kPlain && a.K % 128 != 0)
     hipLaunchKernelGGL((k_f8_tile<MODE, NT, S, MODE == kPlain>), g, b, 0, s, a);
@@ -827,7 +830,7 @@ template <int MODE, int NT, int S, int ROWS = kTileRows>
 hipError_t launch_rows(const F8Args& a, int64_t items, hipStream_t s) {
   const int feats = MODE == kUp ? ROWS / 2 : ROWS;
   const int64_t grid = items * tiles(a.N, feats);
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  if (!one_launch(grid, 2 * ROWS)) return hipErrorInvalidConfiguration;
   const dim3 g(static_cast<uint32_t>(grid)), b(2 * ROWS);
   if (MODE == kPlain && a.K % 128 != 0)
     hipLaunchKernelGGL((k_f8_rows<MODE, NT, S, MODE == kPlain, ROWS>), g, b, 0, s, a);
@@ -979,7 +982,7 @@ __global__ __launch_bounds__(512) void k_f8_mid(F8Args a) {
 template <int S>
 hipError_t launch_mid(const F8Args& a, hipStream_t s) {
   const int64_t grid = tiles(a.N, 64) * tiles(a.M, 64);
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  if (!one_launch(grid, 512)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((k_f8_mid<S>), dim3(static_cast<uint32_t>(grid)), dim3(512), 0, s, a);
   return hipGetLastError();
 }
@@ -1048,6 +1051,10 @@ extern "C" oled_status oled_fp8_matmul(const void* a_dev, const float* a_scale_d
     e = launch_tile<kPlain, 4, 2>(a, tiles(M, 256), s);
   else
     e = launch_tile<kPlain, 2, 3>(a, tiles(M, 128), s);
+  if (e == hipErrorInvalidConfiguration) {
+    set_noctx_error("oled_fp8_matmul: M and N have more tiles than a launch takes");
+    return OLED_ERR_UNSUPPORTED;
+  }
   if (e != hipSuccess) {
     set_noctx_error("oled_fp8_matmul: launch failed");
     return OLED_ERR_HIP;
