@@ -613,7 +613,8 @@ typedef struct {
  *  nonfinite_dev: NULL, or an int32 written 1 if a logit that was looked at is
  *  NaN or infinite, else 0 (such a token still gets k distinct experts; its
  *  weights are unspecified). workspace_dev: at least
- *  oled_route_scored_workspace(T, E) bytes. Calls that share it must not overlap.
+ *  oled_route_scored_workspace(T, E) bytes (which never falls as T grows: a workspace
+ *  for T tokens serves fewer). Calls that share it must not overlap.
  *  Errors: INVALID_ARG (NULL pointers, fields out of range, a short
  *  workspace), UNSUPPORTED (T > 65535, E > 256, k > 16, G no power of two up
  *  to 32).

@@ -656,7 +656,8 @@ __global__ void k_gate_clear(int32_t* bad) { *bad = 0; }
 
 // Tokens of a chunk: 16 while that gives the chip no more than two workgroups a CU. us of a
 // call, 256 experts, 16 against 64: 512 tokens 10.2 : 14.8, 4096 12.3 : 17.0, 8192 16.4 : 18.4.
-int gate_per(int T) { return T <= 8192 ? 16 : kGateChunkMax; }
+constexpr int kGateShort = 8192;   // tokens up to which a chunk has 16
+int gate_per(int T) { return T <= kGateShort ? 16 : kGateChunkMax; }
 int gate_chunks(int T) { return (T + gate_per(T) - 1) / gate_per(T); }
 static_assert((65535 + kGateChunkMax - 1) / kGateChunkMax <= kScanParts * kScanPer, "a thread's chunks");
 
@@ -747,7 +748,11 @@ hipError_t launch_gate(const GateArgs& a, hipStream_t s) {
 
 extern "C" size_t oled_route_scored_workspace(int32_t T, int32_t E) {
   if (T < 1 || E < 1) return 0;
-  return sizeof(int32_t) * static_cast<size_t>(E) * (oled::gate_chunks(T) + 1);
+  // what T tokens need and any number below T
+  int chunks = oled::gate_chunks(T);
+  if (T > oled::kGateShort && chunks < oled::gate_chunks(oled::kGateShort))
+    chunks = oled::gate_chunks(oled::kGateShort);
+  return sizeof(int32_t) * static_cast<size_t>(E) * (chunks + 1);
 }
 
 extern "C" oled_status oled_route_scored(const oled_router* router, const void* logits_dev,
