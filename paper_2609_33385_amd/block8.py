@@ -1,9 +1,9 @@
 """One transformer block's MoE half on 8-bit weights, from the library's calls:
 
-    x += norm(attention output  W_o^T)          oled_norm_in, oled_fp8_matmul, oled_norm_out
-    q  = norm(x) in 8 bits                      oled_norm_in
+    x1 = x + norm(attention output  W_o^T)      oled_norm_in, oled_fp8_matmul, oled_norm_out
+    q  = norm(x1) in 8 bits                     oled_norm_in
     routes of the gate's logits q W_g^T         oled_fp8_matmul, oled_route_scored
-    x += norm(sum_j w_j expert_j(q))            oled_fp8_experts, oled_norm_out
+    x  = x1 + norm(sum_j w_j expert_j(q))       oled_fp8_experts, oled_norm_out
 
 A block owns its weights and its buffers (laid out once, for up to max_tokens), so
 that a call makes eight library calls on one stream and nothing else, and can be
@@ -57,7 +57,8 @@ def _run(status: int, call: str) -> None:
 
 
 class Block8:
-    """forward(x, attn, ...) adds the block to x [T][H] bf16 in place."""
+    """forward(x, attn, ...) adds the block to x [T][H] bf16 in place. Only its last
+    call writes x: where any call is refused, x is as it was."""
 
     def __init__(self, router: oled.Router, hidden: int, inter: int, max_tokens: int,
                  w_out, w_gate, experts: torch.Tensor, slot_of: torch.Tensor | None = None,
@@ -85,6 +86,7 @@ class Block8:
         self.q = torch.zeros((T, hidden), dtype=torch.uint8, device=dev)
         self.q_scale = torch.zeros((T, -(-hidden // 128)), dtype=torch.float32, device=dev)
         self.f = torch.zeros((T, hidden), dtype=torch.bfloat16, device=dev)
+        self.x1 = torch.zeros((T, hidden), dtype=torch.bfloat16, device=dev)
         self.logits = torch.zeros((T, E), dtype=torch.bfloat16, device=dev)
         self.topk_idx, self.weights = ints(T, k), torch.zeros((T, k), device=dev)
         self.counts, self.offsets = ints(E), ints(E + 1)
@@ -114,9 +116,9 @@ class Block8:
         _run(oled.oled_fp8_matmul(self.q, self.q_scale, H, *self.w_out, H, T, H, H, self.f, H, s),
              "oled_fp8_matmul")
         _run(oled.oled_norm_out(self.f, "bf16", None, None, 0, T, H, self.norm_attn, self.eps, None, 0,
-                                x, residual_scale, x, "bf16", s), "oled_norm_out")
+                                x, residual_scale, self.x1, "bf16", s), "oled_norm_out")
         # the experts
-        _run(oled.oled_norm_in(x, "bf16", H, T, H, self.norm_in, self.eps, None, self.q, self.q_scale, s),
+        _run(oled.oled_norm_in(self.x1, "bf16", H, T, H, self.norm_in, self.eps, None, self.q, self.q_scale, s),
              "oled_norm_in")
         _run(oled.oled_fp8_matmul(self.q, self.q_scale, H, *self.w_gate, H, T, E, H, self.logits, E, s),
              "oled_fp8_matmul")
@@ -127,7 +129,7 @@ class Block8:
                                    self.experts, self.experts.shape[0], self.slot_of, self.routed,
                                    self.expert_ws, s), "oled_fp8_experts")
         _run(oled.oled_norm_out(self.routed, "bf16", self.weights, self.inv_perm, k, T, H, self.norm_out,
-                                self.eps, gate, gate_tokens, x, residual_scale, x, "bf16", s),
+                                self.eps, gate, gate_tokens, self.x1, residual_scale, x, "bf16", s),
              "oled_norm_out")
         return x
 

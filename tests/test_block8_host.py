@@ -1,0 +1,90 @@
+"""The chained block's host side: its library calls replaced by stand-ins on the CPU."""
+import pytest
+import torch
+
+from paper_2609_33385_amd import block8, oled
+
+H, I, E, K, TOKENS = 256, 128, 16, 4, 64
+CALLS = ["oled_norm_in", "oled_fp8_matmul", "oled_norm_out", "oled_norm_in", "oled_fp8_matmul",
+         "oled_route_scored", "oled_fp8_experts", "oled_norm_out"]
+OUTPUT = {"oled_norm_in": 8, "oled_fp8_matmul": 9, "oled_norm_out": 13, "oled_route_scored": 5,
+          "oled_fp8_experts": 12}
+
+
+class Stream:
+    """As much of torch.cuda.Stream as the block uses; events are the stream's name."""
+
+    def __init__(self, name, log):
+        self.name, self.log, self.cuda_stream = name, log, hash(name) % 1000 + 1
+
+    def record_event(self):
+        self.log.append(("record", self.name))
+        return self.name
+
+    def wait_event(self, event):
+        self.log.append(("wait", self.name, event))
+
+
+@pytest.fixture
+def stage(monkeypatch):
+    """(log, fail): the calls made, and the index of one that is refused."""
+    log, fail = [], []
+
+    def stand_in(name):
+        def call(*args):
+            stream, out = args[-1], args[OUTPUT[name]]
+            refused = len([c for c in log if c[0] == "call"]) in fail
+            log.append(("call", name, stream.name if stream is not None else None))
+            if refused:
+                return oled.OLED_ERR_UNSUPPORTED
+            out.zero_()
+            return oled.OLED_OK
+        return call
+    for name in OUTPUT:
+        monkeypatch.setattr(oled, name, stand_in(name))
+    made = Stream("made", log)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: made)
+    return log, fail
+
+
+def weights(rows, cols):
+    nb = -(-rows // 128)
+    return torch.zeros((rows, cols), dtype=torch.uint8), torch.ones((nb, cols // 128))
+
+
+def make(tokens=TOKENS, **kw):
+    router = oled.Router(n_experts=E, top_k=K, n_groups=4, top_groups=2, group_best=2, score=1, renorm=1, scale=1.0)
+    experts = torch.zeros((E, oled.oled_fp8_expert_bytes(H, I)), dtype=torch.uint8)
+    return block8.Block8(router, H, I, tokens, weights(H, H), weights(E, H), experts, **kw)
+
+
+def rows(T, value=3.0):
+    return torch.full((T, H), value, dtype=torch.bfloat16)
+
+
+def test_calls(stage):
+    log, _ = stage
+    x = rows(5)
+    assert make().forward(x, rows(5), stream=Stream("a", log)) is x
+    assert [c[1:] for c in log if c[0] == "call"] == [(n, "a") for n in CALLS]
+    assert (x == 0).all()      # the last call's output
+
+
+@pytest.mark.parametrize("at", range(8))
+def test_refused_call_leaves_x(stage, at):
+    log, fail = stage
+    block = make()
+    fail.append(at)
+    x = rows(5)
+    with pytest.raises(oled.OledError, match=CALLS[at]):
+        block.forward(x, rows(5), stream=Stream("a", log))
+    assert (x == 3).all()
+    assert len([c for c in log if c[0] == "call"]) == at + 1
+
+
+def test_routing_workspace_serves_fewer_tokens():
+    """A block for many tokens routes any fewer: the workspace it keeps is no smaller
+    than what each number of tokens asks for."""
+    for tokens in (8193, 20000):
+        kept = oled.oled_route_scored_workspace(tokens, E)
+        assert all(oled.oled_route_scored_workspace(T, E) <= kept for T in (1, 64, 4096, 8191, 8192, tokens))
