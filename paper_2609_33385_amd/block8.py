@@ -58,7 +58,13 @@ def _run(status: int, call: str) -> None:
 
 class Block8:
     """forward(x, attn, ...) adds the block to x [T][H] bf16 in place. Only its last
-    call writes x: where any call is refused, x is as it was."""
+    call writes x: where any call is refused, x is as it was.
+
+    All calls of a block use its buffers. A forward on another stream than the last
+    one's (the first: than the stream the block was made on) therefore waits for what
+    that stream was given so far. Not while it is recorded in a graph: a caller orders
+    the replays of a graph against other forwards of its block, and keeps the block
+    while the graph is used."""
 
     def __init__(self, router: oled.Router, hidden: int, inter: int, max_tokens: int,
                  w_out, w_gate, experts: torch.Tensor, slot_of: torch.Tensor | None = None,
@@ -80,22 +86,43 @@ class Block8:
         self.norm_attn, self.norm_out = norm_attn, norm_out
 
         def ints(*n):
-            return torch.zeros(n, dtype=torch.int32, device=dev)
+            return torch.empty(n, dtype=torch.int32, device=dev)
 
+        # each call writes what the ones after it read
         T, routes = max_tokens, max_tokens * k
-        self.q = torch.zeros((T, hidden), dtype=torch.uint8, device=dev)
-        self.q_scale = torch.zeros((T, -(-hidden // 128)), dtype=torch.float32, device=dev)
-        self.f = torch.zeros((T, hidden), dtype=torch.bfloat16, device=dev)
-        self.x1 = torch.zeros((T, hidden), dtype=torch.bfloat16, device=dev)
-        self.logits = torch.zeros((T, E), dtype=torch.bfloat16, device=dev)
-        self.topk_idx, self.weights = ints(T, k), torch.zeros((T, k), device=dev)
+        self.q = torch.empty((T, hidden), dtype=torch.uint8, device=dev)
+        self.q_scale = torch.empty((T, -(-hidden // 128)), dtype=torch.float32, device=dev)
+        self.f = torch.empty((T, hidden), dtype=torch.bfloat16, device=dev)
+        self.x1 = torch.empty((T, hidden), dtype=torch.bfloat16, device=dev)
+        self.logits = torch.empty((T, E), dtype=torch.bfloat16, device=dev)
+        self.topk_idx, self.weights = ints(T, k), torch.empty((T, k), device=dev)
         self.counts, self.offsets = ints(E), ints(E + 1)
         self.perm, self.inv_perm = ints(routes), ints(routes)
-        self.routed = torch.zeros((routes, hidden), dtype=torch.bfloat16, device=dev)
-        self.route_ws = torch.zeros(oled.oled_route_scored_workspace(T, E), dtype=torch.uint8,
+        self.routed = torch.empty((routes, hidden), dtype=torch.bfloat16, device=dev)
+        self.route_ws = torch.empty(oled.oled_route_scored_workspace(T, E), dtype=torch.uint8,
                                     device=dev)
-        self.expert_ws = torch.zeros(oled.oled_fp8_experts_workspace(T, k, E, hidden, inter),
+        self.expert_ws = torch.empty(oled.oled_fp8_experts_workspace(T, k, E, hidden, inter),
                                      dtype=torch.uint8, device=dev)
+        self.last = torch.cuda.current_stream()   # of the last call
+        self.streams = {self.last.cuda_stream}    # of all calls
+
+    def _after_last(self, stream) -> None:
+        """What `stream` is given from here on comes after the block's last call."""
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream)
+        if stream.cuda_stream == self.last.cuda_stream:
+            return
+        with torch.cuda.stream(stream):
+            if torch.cuda.is_current_stream_capturing():
+                return
+        stream.wait_event(self.last.record_event())
+        if stream.cuda_stream not in self.streams:   # memory is given back after its work too
+            for held in vars(self).values():
+                for t in held if isinstance(held, tuple) else (held,):
+                    if isinstance(t, torch.Tensor):
+                        t.record_stream(stream)
+            self.streams.add(stream.cuda_stream)
+        self.last = stream
 
     def forward(self, x: torch.Tensor, attn: torch.Tensor, token_mask: torch.Tensor | None = None,
                 gate: torch.Tensor | None = None, gate_tokens: int = 0, residual_scale: float = 1.0,
@@ -110,6 +137,7 @@ class Block8:
                 or not (x.is_contiguous() and attn.is_contiguous()):
             raise ValueError("x and attn must be contiguous bf16")
         s = stream if stream is not None else torch.cuda.current_stream()
+        self._after_last(s)
         # the attention's output projection, onto the residual
         _run(oled.oled_norm_in(attn, "bf16", H, T, H, None, self.eps, None, self.q, self.q_scale, s),
              "oled_norm_in")

@@ -1,4 +1,6 @@
 """The chained block's host side: its library calls replaced by stand-ins on the CPU."""
+import contextlib
+
 import pytest
 import torch
 
@@ -9,6 +11,10 @@ CALLS = ["oled_norm_in", "oled_fp8_matmul", "oled_norm_out", "oled_norm_in", "ol
          "oled_route_scored", "oled_fp8_experts", "oled_norm_out"]
 OUTPUT = {"oled_norm_in": 8, "oled_fp8_matmul": 9, "oled_norm_out": 13, "oled_route_scored": 5,
           "oled_fp8_experts": 12}
+
+
+class Stage(tuple):
+    pass
 
 
 class Stream:
@@ -43,8 +49,21 @@ def stage(monkeypatch):
     for name in OUTPUT:
         monkeypatch.setattr(oled, name, stand_in(name))
     made = Stream("made", log)
+    capturing = []      # names of streams under capture
+    within = []
+
+    @contextlib.contextmanager
+    def on(stream):
+        within.append(stream.name)
+        yield
+        within.pop()
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: made)
-    return log, fail
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: within[-1] in capturing)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: log.append(("held", s.name, t.data_ptr())))
+    log_and_fail = Stage((log, fail))
+    log_and_fail.capturing = capturing
+    return log_and_fail
 
 
 def weights(rows, cols):
@@ -88,3 +107,45 @@ def test_routing_workspace_serves_fewer_tokens():
     for tokens in (8193, 20000):
         kept = oled.oled_route_scored_workspace(tokens, E)
         assert all(oled.oled_route_scored_workspace(T, E) <= kept for T in (1, 64, 4096, 8191, 8192, tokens))
+
+
+def order(log):
+    """Waits, and where calls run, each run of calls once."""
+    out = []
+    for c in log:
+        c = c[:3] if c[0] == "wait" else (c[0], c[-1]) if c[0] == "call" else None
+        if c and (not out or out[-1] != c):
+            out.append(c)
+    return out
+
+
+def test_streams_follow_each_other(stage):
+    """A call on another stream waits for the stream of the one before (the first: for the
+    stream the block was made on); calls on one stream add nothing."""
+    log, _ = stage
+    a, b = Stream("a", log), Stream("b", log)
+    block = make(bias=torch.zeros(E))
+    for s in (a, a, b, a, None):
+        block.forward(rows(3), rows(3), stream=s)
+    assert order(log) == [("wait", "a", "made"), ("call", "a"), ("wait", "b", "a"), ("call", "b"),
+                          ("wait", "a", "b"), ("call", "a"), ("wait", "made", "a"), ("call", "made")]
+    for name in ("a", "b"):      # every tensor is held for each stream, once
+        held = [c[2] for c in log if c[:2] == ("held", name)]
+        assert len(held) == len(set(held))
+        for t in (*block.w_out, *block.w_gate, block.experts, block.bias, block.norm_in, block.q, block.q_scale,
+                  block.f, block.x1, block.logits, block.topk_idx, block.weights, block.counts, block.offsets,
+                  block.perm, block.inv_perm, block.routed, block.route_ws, block.expert_ws):
+            assert t.data_ptr() in held
+
+
+def test_no_wait_while_recorded(stage):
+    """A stream under capture cannot wait for work outside of it; the next call that is
+    not recorded follows the last one that was not."""
+    log, _ = stage
+    a, b, g = Stream("a", log), Stream("b", log), Stream("g", log)
+    stage.capturing.append("g")
+    block = make()
+    for s in (a, g, a, g, b):
+        block.forward(rows(3), rows(3), stream=s)
+    assert order(log) == [("wait", "a", "made"), ("call", "a"), ("call", "g"), ("call", "a"), ("call", "g"),
+                          ("wait", "b", "a"), ("call", "b")]
