@@ -56,6 +56,15 @@ def _run(status: int, call: str) -> None:
         raise oled.OledError(status, f"{call}: {oled.last_error(None)}")
 
 
+def _check(t: torch.Tensor, what: str, dtype, least: int, device) -> None:
+    """t holds at least `least` values of dtype (an int: of that many bytes), in order, on the device."""
+    right = t.element_size() == dtype if isinstance(dtype, int) else t.dtype == dtype
+    if not (right and t.numel() >= least and t.is_contiguous() and t.device == device):
+        raise ValueError(f"{what} must be contiguous, on {device}, {least} values of "
+                         f"{f'{dtype} byte' if isinstance(dtype, int) else dtype}: it is {tuple(t.shape)} of "
+                         f"{t.dtype} on {t.device}")
+
+
 class Block8:
     """forward(x, attn, ...) adds the block to x [T][H] bf16 in place. Only its last
     call writes x: where any call is refused, x is as it was.
@@ -74,7 +83,8 @@ class Block8:
         """w_out, w_gate: (e4m3, scales) of W_o [H][H] and the gate [E][H]
         (quantise); experts: packed blocks; slot_of [E] int32: the block of each
         expert (None: block e); bias [E] fp32: the router's balance bias; norm_*
-        [H] fp32 (None for norm_attn and norm_out: that output has no norm)."""
+        [H] fp32 (None for norm_attn and norm_out: that output has no norm). ValueError
+        where a size is not one that the calls take or a tensor is too short for it."""
         E, k = router.n_experts, router.top_k
         self.router = oled.Router.from_buffer_copy(router)   # its logits are the block's own, in bf16
         self.hidden, self.inter, self.max_tokens = hidden, inter, max_tokens
@@ -84,6 +94,22 @@ class Block8:
         dev = experts.device
         self.norm_in = norm_in if norm_in is not None else torch.ones(hidden, device=dev)
         self.norm_attn, self.norm_out = norm_attn, norm_out
+        if not 1 <= max_tokens <= 65535 or any(n % 128 or not 128 <= n <= 16384 for n in (hidden, inter)):
+            raise ValueError("max_tokens must be in [1, 65535], hidden and inter multiples of 128 up to 16384")
+        blocks = hidden // 128
+        for w, what, rows in ((w_out, "w_out", hidden), (w_gate, "w_gate", E)):
+            _check(w[0], what, 1, rows * hidden, dev)
+            _check(w[1], f"{what}'s scales", torch.float32, -(-rows // 128) * blocks, dev)
+        size = oled.oled_fp8_expert_bytes(hidden, inter)
+        if experts.dim() != 2 or experts.shape[1] != size:
+            raise ValueError(f"experts must be rows of {size} bytes: they are {tuple(experts.shape)}")
+        _check(experts, "experts", 1, size * (1 if slot_of is not None else E), dev)
+        for v, what, dtype, n in ((slot_of, "slot_of", torch.int32, E), (bias, "bias", torch.float32, E),
+                                  (self.norm_in, "norm_in", torch.float32, hidden),
+                                  (norm_attn, "norm_attn", torch.float32, hidden),
+                                  (norm_out, "norm_out", torch.float32, hidden)):
+            if v is not None:
+                _check(v, what, dtype, n, dev)
 
         def ints(*n):
             return torch.empty(n, dtype=torch.int32, device=dev)
@@ -129,13 +155,21 @@ class Block8:
                 stream=None) -> torch.Tensor:
         """x, attn [T][H] bf16, contiguous; token_mask [T] bool or bytes: tokens
         without routes where 0; gate: fp32 rows of H that scale the MoE output,
-        token t under row t / gate_tokens (row 0 if gate_tokens is 0)."""
+        token t under row t / gate_tokens (row 0 if gate_tokens is 0). ValueError where
+        a tensor is of another type or too short."""
         T, H, k, E = x.shape[0], self.hidden, self.router.top_k, self.router.n_experts
         if not 1 <= T <= self.max_tokens or x.shape != (T, H) or attn.shape != (T, H):
             raise ValueError(f"x and attn must be [1..{self.max_tokens}][{H}]")
         if x.dtype != torch.bfloat16 or attn.dtype != torch.bfloat16 \
                 or not (x.is_contiguous() and attn.is_contiguous()):
             raise ValueError("x and attn must be contiguous bf16")
+        dev = self.experts.device
+        if x.device != dev or attn.device != dev:
+            raise ValueError(f"x and attn must be on {dev}")
+        if token_mask is not None:
+            _check(token_mask, "token_mask", 1, T, dev)
+        if gate is not None:
+            _check(gate, "gate", torch.float32, H * (-(-T // gate_tokens) if gate_tokens > 0 else 1), dev)
         s = stream if stream is not None else torch.cuda.current_stream()
         self._after_last(s)
         # the attention's output projection, onto the residual

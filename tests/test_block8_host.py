@@ -149,3 +149,48 @@ def test_no_wait_while_recorded(stage):
         block.forward(rows(3), rows(3), stream=s)
     assert order(log) == [("wait", "a", "made"), ("call", "a"), ("call", "g"), ("call", "a"), ("call", "g"),
                           ("wait", "b", "a"), ("call", "b")]
+
+
+F32, I32, U8, BF16 = torch.float32, torch.int32, torch.uint8, torch.bfloat16
+
+
+@pytest.mark.parametrize("change", [
+    dict(token_mask=torch.ones(4, dtype=U8)), dict(token_mask=torch.ones(5, dtype=torch.int64)),
+    dict(token_mask=torch.ones(10, dtype=U8)[::2]), dict(gate=torch.ones(H - 1)), dict(gate=torch.ones(H).double()),
+    dict(gate=torch.ones((2, H)), gate_tokens=2), dict(gate=torch.ones((H, 2)).t()[0]),
+    dict(gate=torch.ones((1, H), dtype=BF16)), dict(gate=torch.ones((4, H)), gate_tokens=1)])
+def test_short_or_wrong_call_arguments(stage, change):
+    """Refused before any call is made; x is as it was."""
+    log, _ = stage
+    block, x = make(), rows(5)
+    with pytest.raises(ValueError, match="must be contiguous"):
+        block.forward(x, rows(5), stream=Stream("a", log), **change)
+    assert not log and (x == 3).all()
+
+
+@pytest.mark.parametrize("change", [
+    dict(token_mask=torch.ones(5, dtype=torch.bool)), dict(token_mask=torch.ones(9, dtype=U8)),
+    dict(gate=torch.ones(H)), dict(gate=torch.ones((1, H))), dict(gate=torch.ones((3, H)), gate_tokens=2),
+    dict(gate=torch.ones((1, H)), gate_tokens=5), dict(gate=torch.ones((1, H)), gate_tokens=500)])
+def test_right_call_arguments(stage, change):
+    log, _ = stage
+    make().forward(rows(5), rows(5), stream=Stream("a", log), **change)
+    assert len([c for c in log if c[0] == "call"]) == 8
+
+
+@pytest.mark.parametrize("change", [
+    dict(bias=torch.zeros(E - 1)), dict(bias=torch.zeros(E, dtype=BF16)), dict(slot_of=torch.zeros(E)),
+    dict(slot_of=torch.zeros(E - 1, dtype=I32)), dict(norm_in=torch.ones(H - 8)), dict(norm_attn=torch.ones(8)),
+    dict(norm_out=torch.ones(H).double()), dict(norm_out=torch.ones(2 * H)[::2]), dict(tokens=0), dict(tokens=65536),
+    dict(hidden=200), dict(inter=64), dict(hidden=1 << 15), dict(w_out=weights(128, H)), dict(w_gate=weights(8, H)),
+    dict(w_out=(torch.zeros((H, H)), torch.ones((2, 2)))), dict(w_gate=(torch.zeros((E, H), dtype=U8), torch.ones(1))),
+    dict(experts=torch.zeros((E, 256), dtype=U8)), dict(experts=torch.zeros(9, dtype=U8)), dict(blocks=E - 1)])
+def test_short_or_wrong_parts(stage, change):
+    router = oled.Router(n_experts=E, top_k=K, n_groups=4, top_groups=2, group_best=2, score=1, renorm=1, scale=1.0)
+    size = oled.oled_fp8_expert_bytes(H, I)
+    part = dict(hidden=H, inter=I, tokens=8, w_out=weights(H, H), w_gate=weights(E, H),
+                experts=torch.zeros((change.pop("blocks", E), size), dtype=U8))
+    part.update(change)
+    args = [part.pop(n) for n in ("hidden", "inter", "tokens", "w_out", "w_gate", "experts")]
+    with pytest.raises(ValueError, match="must be"):
+        block8.Block8(router, *args, **part)
