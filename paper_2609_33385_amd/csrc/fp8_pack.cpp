@@ -48,10 +48,12 @@ void pack(int rows, int cols, Get&& get, uint8_t* q, float* scale) {
     }
 }
 
+bool supported(int n) { return n >= 128 && n <= 16384 && n % 128 == 0; }
+
 }  // namespace
 
 extern "C" size_t oled_fp8_expert_bytes(int32_t hidden, int32_t inter) {
-  if (hidden < 128 || inter < 128 || hidden % 128 != 0 || inter % 128 != 0) return 0;
+  if (!supported(hidden) || !supported(inter)) return 0;
   const size_t n = static_cast<size_t>(hidden) * inter;
   return (3 * n + 12 * (n / 16384) + 255) / 256 * 256;
 }
@@ -60,9 +62,7 @@ extern "C" oled_status oled_fp8_pack_expert(int32_t dtype, int32_t hidden, int32
                                             const void* w13, const void* w2, void* block_out) {
   if (!w13 || !w2 || !block_out || (dtype != OLED_F32 && dtype != OLED_BF16))
     return OLED_ERR_INVALID_ARG;
-  if (hidden < 128 || inter < 128 || hidden % 128 != 0 || inter % 128 != 0 || hidden > 16384 ||
-      inter > 16384)
-    return OLED_ERR_UNSUPPORTED;
+  if (!supported(hidden) || !supported(inter)) return OLED_ERR_UNSUPPORTED;
   const size_t HI = static_cast<size_t>(hidden) * inter;
   uint8_t* q = static_cast<uint8_t*>(block_out);
   float* s = reinterpret_cast<float*>(q + 3 * HI);
