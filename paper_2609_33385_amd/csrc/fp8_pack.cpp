@@ -3,6 +3,7 @@
 #include <cstdint>
 #include <cstring>
 
+#include "kernels.h"
 #include "oled.h"
 
 namespace {
@@ -60,9 +61,14 @@ extern "C" size_t oled_fp8_expert_bytes(int32_t hidden, int32_t inter) {
 
 extern "C" oled_status oled_fp8_pack_expert(int32_t dtype, int32_t hidden, int32_t inter,
                                             const void* w13, const void* w2, void* block_out) {
-  if (!w13 || !w2 || !block_out || (dtype != OLED_F32 && dtype != OLED_BF16))
+  if (!w13 || !w2 || !block_out || (dtype != OLED_F32 && dtype != OLED_BF16)) {
+    oled::set_noctx_error("oled_fp8_pack_expert: NULL weights or block, or bad dtype");
     return OLED_ERR_INVALID_ARG;
-  if (!supported(hidden) || !supported(inter)) return OLED_ERR_UNSUPPORTED;
+  }
+  if (!supported(hidden) || !supported(inter)) {
+    oled::set_noctx_error("oled_fp8_pack_expert: H and I must be multiples of 128 up to 16384");
+    return OLED_ERR_UNSUPPORTED;
+  }
   const size_t HI = static_cast<size_t>(hidden) * inter;
   uint8_t* q = static_cast<uint8_t*>(block_out);
   float* s = reinterpret_cast<float*>(q + 3 * HI);

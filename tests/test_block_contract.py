@@ -3,6 +3,8 @@ import pytest
 
 from paper_2609_33385_amd import oled
 
+P = 1 << 20     # a pointer that is never read
+
 
 @pytest.mark.parametrize("H,I", [(16512, 128), (128, 16512), (32768, 32768), (1 << 30, 128), (0, 128), (128, 0), (192, 128)])
 def test_bytes_of_unsupported_shapes(H, I):
@@ -11,3 +13,14 @@ def test_bytes_of_unsupported_shapes(H, I):
 
 def test_bytes_of_the_largest_shape():
     assert oled.oled_fp8_expert_bytes(16384, 16384) == 3 * 2 ** 28 + 12 * 2 ** 14
+
+
+@pytest.mark.parametrize("args,status", [((0, 128, 128, None, P, P), 1), ((0, 128, 128, P, None, P), 1),
+                                         ((0, 128, 128, P, P, None), 1), ((7, 128, 128, P, P, P), 1),
+                                         ((0, 130, 128, P, P, P), 5), ((1, 128, 16512, P, P, P), 5)])
+def test_pack_refusals_leave_their_text(args, status):
+    lib = oled.load()
+    assert lib.oled_norm_in(None, 0, 8, 1, 8, None, 0.0, None, None, None, None) == 1
+    assert "oled_norm_in" in oled.last_error(None)
+    assert lib.oled_fp8_pack_expert(*args) == status
+    assert "oled_fp8_pack_expert" in oled.last_error(None)
