@@ -393,11 +393,17 @@ def oled_fp8_pack_expert(dtype: str, hidden: int, inter: int, w13: np.ndarray, w
     the 8-bit expert block `out` (uint8)."""
     w13 = np.ascontiguousarray(w13)
     w2 = np.ascontiguousarray(w2)
-    assert out.flags.c_contiguous and out.nbytes == oled_fp8_expert_bytes(hidden, inter)
+    size = oled_fp8_expert_bytes(hidden, inter)
+    if size:      # else the shape is refused before anything is read
+        value = {"f32": 4, "bf16": 2}[dtype]
+        for w, name, n in ((w13, "w13", 2 * inter * hidden), (w2, "w2", hidden * inter)):
+            if w.size != n or w.itemsize != value:
+                raise ValueError(f"{name} must be {n} values of {value} bytes: it is {w.shape} of {w.dtype}")
+        assert out.flags.c_contiguous and out.nbytes == size
     st = load().oled_fp8_pack_expert(DTYPES[dtype], hidden, inter, w13.ctypes.data, w2.ctypes.data,
                                      out.ctypes.data)
     if st != OLED_OK:
-        raise OledError(st, "oled_fp8_pack_expert")
+        raise OledError(st, last_error(None))
 
 
 def moe_forward_cached(ctx, layer: int, x, y, stream=None) -> int:

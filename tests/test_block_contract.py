@@ -1,4 +1,5 @@
-"""What the header promises of the 8-bit packing (no GPU)."""
+"""What the header promises of the 8-bit packing and what the binding hands on (no GPU)."""
+import numpy as np
 import pytest
 
 from paper_2609_33385_amd import oled
@@ -24,3 +25,21 @@ def test_pack_refusals_leave_their_text(args, status):
     assert "oled_norm_in" in oled.last_error(None)
     assert lib.oled_fp8_pack_expert(*args) == status
     assert "oled_fp8_pack_expert" in oled.last_error(None)
+
+
+@pytest.mark.parametrize("dtype,w13,w2", [
+    ("f32", ((256, 256), np.float32), ((256, 127), np.float32)), ("f32", ((255, 256), np.float32), ((256, 128), np.float32)),
+    ("f32", ((256, 256), np.float64), ((256, 128), np.float32)), ("f32", ((256, 256), np.float32), ((256, 128), np.uint16)),
+    ("bf16", ((256, 256), np.float32), ((256, 128), np.uint16)), ("bf16", ((256, 256), np.uint16), ((128, 128), np.uint16))])
+def test_pack_checks_its_arrays(dtype, w13, w2):
+    """Weights of another size or type are refused, not read past their end."""
+    out = np.full(oled.oled_fp8_expert_bytes(256, 128), 0xEE, np.uint8)
+    with pytest.raises(ValueError, match="w13|w2"):
+        oled.oled_fp8_pack_expert(dtype, 256, 128, np.zeros(*w13), np.zeros(*w2), out)
+    assert (out == 0xEE).all()
+
+
+def test_pack_of_an_unsupported_shape():
+    with pytest.raises(oled.OledError, match="multiples of 128"):
+        oled.oled_fp8_pack_expert("f32", 130, 128, np.zeros((256, 130), np.float32), np.zeros((130, 128), np.float32),
+                                  np.zeros(1 << 18, np.uint8))
