@@ -324,7 +324,7 @@ def oled_priority_batch(topk_idx, gates, conf, B: int, T: int, E: int, k: int, s
 
 
 def _bytes(t) -> int:
-    return t.numel() * t.element_size()
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def oled_route_scored(router: Router, logits, bias, token_mask, T: int, topk_idx, weights, counts,

@@ -43,3 +43,12 @@ def test_pack_of_an_unsupported_shape():
     with pytest.raises(oled.OledError, match="multiples of 128"):
         oled.oled_fp8_pack_expert("f32", 130, 128, np.zeros((256, 130), np.float32), np.zeros((130, 128), np.float32),
                                   np.zeros(1 << 18, np.uint8))
+
+
+def test_no_workspace_is_a_status():
+    """A missing workspace is the library's refusal, as any missing array is."""
+    r = oled.Router(n_experts=64, top_k=8, n_groups=1, top_groups=1, group_best=1, score=1, renorm=1, dtype=0, scale=1.0)
+    assert oled.oled_route_scored(r, P, None, None, 4, P, P, P, P, P, P, None, None) == oled.OLED_ERR_INVALID_ARG
+    assert "oled_route_scored" in oled.last_error(None)
+    assert oled.oled_fp8_experts(P, P, P, P, 4, 2, 8, 256, 128, P, 8, None, P, None) == oled.OLED_ERR_INVALID_ARG
+    assert "oled_fp8_experts" in oled.last_error(None)
