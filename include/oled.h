@@ -571,8 +571,10 @@ oled_status oled_priority_batch(const int32_t* topk_idx_dev, const float* gates_
  * be captured. 8-bit values are OCP e4m3 (no infinities). A quantised row x has
  * one fp32 scale for each 128 consecutive values, s = max(amax, 2^-100) / 448
  * and q = x / s rounded to nearest even (a NaN stays a NaN; values beside an
- * infinity are lost); a quantised matrix has one for each 128 x 128 block, both
- * sides counted from its first row and column (a last block may be short).
+ * infinity are lost): on the device the fp32 product x (1 / s), in
+ * oled_fp8_pack_expert the quotient, which can round apart at a midpoint. A
+ * quantised matrix has one for each 128 x 128 block, both sides counted from its
+ * first row and column (a last block may be short).
  * Errors of these calls: INVALID_ARG, UNSUPPORTED, HIP, with the text in
  * oled_last_error(NULL). They come from the host's checks or from a launch
  * that failed, before any work of the call has run in the first two cases.
@@ -596,13 +598,15 @@ typedef struct {
 
 /*
  * oled_route_scored: routes T tokens by scores s[e] = 1 / (1 + exp(-l[e])) or
- *  softmax(l)[e], in fp32. An expert's choice value is s[e] + bias[e] (a
- *  balance bias, on the choice alone). Without a bias it is s[e] where group_best
- *  is 2 (also where all groups compete), else l[e], which is in the same order but
- *  keeps apart what saturated scores do not. The top_groups
- *  groups of the largest values compete, then the k largest choice values, in
- *  falling order; equal ones go to the lower group or expert. weight[t][j] =
- *  scale * s[e_j] / (sum_j s[e_j] + 1e-20), or scale * s[e_j] without renorm.
+ *  softmax(l)[e], in fp32: exp and 1 / x are the unit's instructions, so a score is
+ *  off by some (8 + 2 d) 2^-24 of itself, d the spread of the token's logits
+ *  (sigmoid: |l|), softmax by E 2^-24 more. An expert's choice value is s[e] +
+ *  bias[e] (a balance bias, on the choice alone). Without a bias it is s[e] where
+ *  group_best is 2 (also where all groups compete), else l[e], which is in the same
+ *  order but keeps apart what saturated scores do not. The top_groups groups of the
+ *  largest values compete, then the k largest choice values, in falling order;
+ *  equal ones go to the lower group or expert. weight[t][j] = scale * s[e_j] /
+ *  (sum_j s[e_j] + 1e-20), or scale * s[e_j] without renorm.
  *  Then the histogram, offsets and permutation of the routes by (expert, token).
  *  logits_dev [T][E] of router->dtype; bias_dev [E] fp32 or NULL;
  *  token_mask_dev [T] bytes or NULL: a token whose byte is 0 has no routes (its
@@ -629,9 +633,9 @@ size_t oled_route_scored_workspace(int32_t T, int32_t E);
 
 /*
  * oled_norm_in: the norm in front of a block, n = x rsqrt(mean(x^2) + eps) w,
- *  row by row, sums in fp32; where mean(x^2) + eps is 0 (a row of zeros, or of values whose
- *  squares are below fp32, with eps 0) n = 0. x_dev [T] rows of H in dtype, ldx elements apart;
- *  weight_dev [H] fp32, or NULL: the rows as they are (n = x). n_dev [T][H] in
+ *  row by row, sums in fp32; where mean(x^2) + eps is 0 (eps 0 and a row of zeros, or
+ *  of values whose squares are below fp32) n = 0. x_dev [T] rows of H in dtype, ldx
+ *  elements apart; weight_dev [H] fp32, or NULL: the rows as they are (n = x). n_dev [T][H] in
  *  dtype, or NULL; q_dev [T][H] e4m3 of the unrounded n with q_scale_dev
  *  [T][ceil(H / 128)] fp32, or both NULL.
  *  Errors: INVALID_ARG (NULL x, no output, T or H < 1, ldx < H, eps < 0 or

@@ -87,6 +87,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {   // v_cvt_p
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2_t{lo, hi}, bf16x2_t));
 }
 
+// exp by v_exp_f32, within some 2 + |v| units of 2^-24: h is rounded to 8 bits next.
+__device__ __forceinline__ float silu(float v) { return v / (1.f + __expf(-v)); }
+
 int64_t tiles(int n, int size) { return (static_cast<int64_t>(n) - 1) / size + 1; }
 
 // A launch takes fewer than 2^32 threads; the grid of a larger one would wrap, without an error.
@@ -646,7 +649,7 @@ __device__ __forceinline__ void run_tile(const F8Args& a, const Item& it, int we
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float v = acc[i][n][r];
-          h[i][n][r] = v / (1.f + __expf(-v)) * acc[4 + i][n][r];
+          h[i][n][r] = silu(v) * acc[4 + i][n][r];
           m = fmaxf(m, fabsf(h[i][n][r]));
         }
       m = fmaxf(m, __shfl_xor(m, 16));
@@ -800,7 +803,7 @@ __global__ __launch_bounds__(2 * ROWS, ROWS / 64) void k_f8_rows(F8Args a) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float v = acc[0][n][r];
-        h[n][r] = v / (1.f + __expf(-v)) * acc[1][n][r];
+        h[n][r] = silu(v) * acc[1][n][r];
         m = fmaxf(m, fabsf(h[n][r]));
       }
       m = fmaxf(m, __shfl_xor(m, 16));
@@ -843,8 +846,8 @@ hipError_t launch_rows(const F8Args& a, int64_t items, hipStream_t s) {
 // Products with too few tiles of 256 rows for the chip: a workgroup takes 64 weight
 // rows x 64 token rows and stages of 256 of K, 4 wavefronts (2 x 2 of 32 x 32) on
 // either half of a stage; the halves are added at the end. Bound by the latency of its
-// steps: 256 x 4096 x 4096 11.4 us (1.5 TB/s, 750 TFLOP/s), 257 x 2049 x 2000 8.8 us of
-// which a launch and the first stage are half.
+// steps: 256 x 4096 x 4096 11.7 us (1.5 TB/s, 730 TFLOP/s; 0.25 of them the question which
+// scales are there), 257 x 2049 x 2000 8.8 us of which a launch and the first stage are half.
 constexpr int kMidStage = 2 * 128 * 128;   // bytes: two halves of 64 weight and 64 token rows
 
 template <int S>

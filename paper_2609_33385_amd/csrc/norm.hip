@@ -2,7 +2,9 @@
 //
 //  in   n = x * rsqrt(mean(x^2) + eps) * w, rounded to x's dtype for the gate, and
 //       the unrounded n in 8 bits for the experts: e4m3 with a scale
-//       s = max(amax, 2^-100) / 448 for each 128 consecutive values.
+//       s = max(amax, 2^-100) / 448 for each 128 consecutive values, rounded from the
+//       fp32 product n (1 / s) (one reciprocal for 8 values of a lane; a quotient
+//       each would differ at midpoints alone).
 //  out  f_t = sum_j weight[t][j] O[inv_perm[t k + j]] (or a dense row f_t),
 //       y_t = alpha x_t + gate o (f_t * rsqrt(mean(f_t^2) + eps) * w).
 //
